@@ -340,6 +340,10 @@ ism_status_t ism_attn_bwd_rope_planned(const ism_segments_t* segs, const ism_att
  *     (only the bf16 single-token step at head_dim 128 whose caches differ in
  *     length or are short covers all keys then; others stop where the mirror's
  *     last chunk or part ends).
+ *     A device length that leaves no room for the new rows (or is negative) counts
+ *     as the nearest one that does: nothing outside the caches is read or
+ *     written, nothing is written for that sequence, its results are undefined,
+ *     and ism_check_status reports ISM_ERR_INVALID_ARG.
  *   o_new [B, l_new, Hq, D] (dtype, written); lse_new [Hq, B, l_new] fp32 or NULL.
  * If a cache ends inside a query segment its old rows would differ from a
  * full pass once the segment grows; the new rows are still exact.
@@ -394,6 +398,9 @@ ism_status_t ism_attn_prefill_append_e4m3(const ism_attn_shape_t* shape, int32_t
  *   block_table [B, max_pages] int32 device, block_table_host its host mirror:
  *     the pages of sequence b, in key order; entries that cover keys
  *     [0, cache_len[b] + l_new) must lie in [0, num_pages), the rest are not read.
+ *     Where the device's entry of a new row lies outside the pool although the
+ *     mirror's does not, the row is not written and ism_check_status reports
+ *     ISM_ERR_INVALID_ARG; reads stay inside the pool.
  *     Two sequences may share a page only where both only read it.
  *   cache_len / cache_len_host as for ism_attn_prefill_append;
  *     cache_len_host[b] + l_new <= max_pages * page_size is required.
@@ -615,7 +622,9 @@ ism_status_t ism_pages_compact(const ism_pages_t* pages, int32_t* pages_used, is
 /* Synchronises `stream`, then reads and clears the current device's status
  * word.  Returns ISM_ERR_TIMEOUT if any kernel gave up a bounded wait since
  * the last check (the kernel exits early and its outputs are undefined),
- * ISM_ERR_CUDA on a CUDA error, ISM_OK otherwise. */
+ * ISM_ERR_INVALID_ARG if an append found cache lengths or pages on the device
+ * that its host mirrors do not have and left rows out, ISM_ERR_CUDA on a CUDA
+ * error, ISM_OK otherwise. */
 ism_status_t ism_check_status(ism_stream_t stream);
 
 /* Test hook for the bounded-wait machinery: launches one kernel that waits on

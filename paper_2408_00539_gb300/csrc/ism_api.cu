@@ -1195,6 +1195,9 @@ ism_status_t append_impl(const ism_attn_shape_t* shape, int32_t batch, const voi
   if ((r = status_ptr(&status)) != ISM_OK) return r;
   const int hq = shape->num_heads_q, hkv = shape->num_heads_kv, d = shape->head_dim;
   const bool paged = cg.pages.table != nullptr;
+  int64_t keys_most = cg.max_keys < INT32_MAX ? cg.max_keys : INT32_MAX;
+  if (rope && rope->rows < keys_most) keys_most = rope->rows;
+  const CacheLens lens{cache_len, (int32_t)(keys_most - l_new), status};
 
   // decode kernels serve up to kMaxDecodeGroup query heads per KV head; larger
   // groups take the forward kernels (one query row per tile)
@@ -1204,7 +1207,7 @@ ism_status_t append_impl(const ism_attn_shape_t* shape, int32_t batch, const voi
     DecodeArgs w{};
     w.q = q_new; w.k_cache = k_cache; w.v_cache = v_cache; w.pages = cg.pages; w.out = o_new; w.lse = lse_new;
     w.batch = batch; w.hq = hq; w.hkv = hkv; w.d = d; w.dtype = shape->dtype; w.group = hq / hkv;
-    w.cap = cg.cap; w.scale = shape->softmax_scale; w.cache_len = cache_len;
+    w.cap = cg.cap; w.scale = shape->softmax_scale; w.cache_len = cache_len; w.status = status;
     w.win = win.window ? win : Window{max_c + 1, 0};  // (a window that covers all)
     if (decode_window_one_launch(w, cache_len_host)) {
       timer_begin(ISM_KERNEL_DECODE, st);
@@ -1229,13 +1232,13 @@ ism_status_t append_impl(const ism_attn_shape_t* shape, int32_t batch, const voi
   timer_begin(ISM_KERNEL_META, st);
   int32_t* snap_out = decode ? L.c_snap : nullptr;
   if (rope) {
-    ISM_TRY_CUDA(launch_rope_cache_write(shape->dtype, batch, l_new, hq, hkv, d, cg.cap, cg.pages, cache_len, q_new,
+    ISM_TRY_CUDA(launch_rope_cache_write(shape->dtype, batch, l_new, hq, hkv, d, cg.cap, cg.pages, lens, q_new,
                                          k_new, v_new, rope->cos, rope->sin, q_descale, k_descale, v_descale,
                                          L.q_rot, k_cache, v_cache, plan, st, snap_out),
                  "rope cache write launch");
     q_new = L.q_rot;  // the attention below reads the rotated queries
   } else {
-    ISM_TRY_CUDA(launch_cache_write(shape->dtype, batch, l_new, hkv, d, cg.cap, cg.pages, cache_len, k_new, v_new,
+    ISM_TRY_CUDA(launch_cache_write(shape->dtype, batch, l_new, hkv, d, cg.cap, cg.pages, lens, k_new, v_new,
                                     k_cache, v_cache, plan, st, snap_out),
                  "cache write launch");
   }
@@ -1244,6 +1247,7 @@ ism_status_t append_impl(const ism_attn_shape_t* shape, int32_t batch, const voi
   if (decode) {
     DecodeArgs a{};
     a.cache_len = cache_len;
+    a.len_most = lens.most;
     a.q_written = rope != nullptr;
     a.q = q_new; a.k_cache = k_cache; a.v_cache = v_cache; a.pages = cg.pages; a.out = o_new; a.lse = lse_new;
     a.c_snap = L.c_snap;
@@ -1313,6 +1317,7 @@ ism_status_t append_impl(const ism_attn_shape_t* shape, int32_t batch, const voi
   a.adv_cache_len = cache_len;
   a.adv_batch = batch;
   a.adv_len = l_new;
+  a.adv_most = lens.most;
   a.status = status;
   a.flags = tc_flags();
   a.win = win;
@@ -1390,7 +1395,7 @@ ism_status_t ism_attn_prefill_append(const ism_attn_shape_t* shape, int32_t batc
   cg.cap = cache_capacity;
   cg.kv_rows = (int64_t)batch * cache_capacity;
   cg.max_keys = cache_capacity;
-  cg.pages = KvPages{nullptr, 0, 0};
+  cg.pages = KvPages{nullptr, 0, 0, 0};
   return append_impl(shape, batch, q_new, k_new, v_new, l_new, new_seg_end_host, new_seg_type_host, n_new_segs,
                      k_cache, v_cache, cg, cache_len, cache_len_host, o_new, lse_new, workspace, workspace_bytes,
                      reinterpret_cast<cudaStream_t>(stream));
@@ -1417,7 +1422,7 @@ ism_status_t ism_attn_prefill_append_e4m3(const ism_attn_shape_t* shape, int32_t
   cg.cap = cache_capacity;
   cg.kv_rows = (int64_t)batch * cache_capacity;
   cg.max_keys = cache_capacity;
-  cg.pages = KvPages{nullptr, 0, 0};
+  cg.pages = KvPages{nullptr, 0, 0, 0};
   return append_impl(shape, batch, q_new, k_new, v_new, l_new, new_seg_end_host, new_seg_type_host, n_new_segs,
                      k_cache, v_cache, cg, cache_len, cache_len_host, o_new, lse_new, workspace, workspace_bytes,
                      reinterpret_cast<cudaStream_t>(stream), q_descale, k_descale, v_descale);
@@ -1442,7 +1447,7 @@ ism_status_t ism_attn_prefill_append_rope(const ism_attn_shape_t* shape, int32_t
   cg.cap = cache_capacity;
   cg.kv_rows = (int64_t)batch * cache_capacity;
   cg.max_keys = cache_capacity;
-  cg.pages = KvPages{nullptr, 0, 0};
+  cg.pages = KvPages{nullptr, 0, 0, 0};
   return append_impl(shape, batch, q_new, k_new, v_new, l_new, new_seg_end_host, new_seg_type_host, n_new_segs,
                      k_cache, v_cache, cg, cache_len, cache_len_host, o_new, lse_new, workspace, workspace_bytes,
                      reinterpret_cast<cudaStream_t>(stream), 1.f, 1.f, 1.f, rope);
@@ -1471,7 +1476,7 @@ ism_status_t ism_attn_prefill_append_e4m3_rope(const ism_attn_shape_t* shape, in
   cg.cap = cache_capacity;
   cg.kv_rows = (int64_t)batch * cache_capacity;
   cg.max_keys = cache_capacity;
-  cg.pages = KvPages{nullptr, 0, 0};
+  cg.pages = KvPages{nullptr, 0, 0, 0};
   return append_impl(shape, batch, q_new, k_new, v_new, l_new, new_seg_end_host, new_seg_type_host, n_new_segs,
                      k_cache, v_cache, cg, cache_len, cache_len_host, o_new, lse_new, workspace, workspace_bytes,
                      reinterpret_cast<cudaStream_t>(stream), q_descale, k_descale, v_descale, rope);
@@ -1510,7 +1515,7 @@ ism_status_t paged_geom(int32_t batch, int32_t l_new, int32_t num_pages, int32_t
   cg->cap = 0;
   cg->kv_rows = (int64_t)num_pages * page_size;
   cg->max_keys = (int64_t)max_pages * page_size;
-  cg->pages = KvPages{block_table, page_size, max_pages};
+  cg->pages = KvPages{block_table, page_size, max_pages, num_pages};
   return ISM_OK;
 }
 
@@ -1617,7 +1622,7 @@ ism_status_t ism_attn_prefill_append_window(const ism_attn_shape_t* shape, const
   cg.cap = cache_capacity;
   cg.kv_rows = (int64_t)batch * cache_capacity;
   cg.max_keys = cache_capacity;
-  cg.pages = KvPages{nullptr, 0, 0};
+  cg.pages = KvPages{nullptr, 0, 0, 0};
   return append_impl(shape, batch, q_new, k_new, v_new, l_new, new_seg_end_host, new_seg_type_host, n_new_segs,
                      k_cache, v_cache, cg, cache_len, cache_len_host, o_new, lse_new, workspace, workspace_bytes,
                      reinterpret_cast<cudaStream_t>(stream), 1.f, 1.f, 1.f, rope, window);
@@ -1665,6 +1670,9 @@ ism_status_t ism_check_status(ism_stream_t stream) {
   if (word & kStatusTimeout) return fail(ISM_ERR_TIMEOUT, "a device-side wait gave up (status word 0x%x)", word);
   if (word & kStatusSmemAlign)
     return fail(ISM_ERR_CUDA, "a kernel found its shared memory misaligned and skipped its work (0x%x)", word);
+  if (word & kStatusCache)
+    return fail(ISM_ERR_INVALID_ARG, "an append found a cache length or a page on the device that the host's mirrors do not "
+                "have (0x%x): its rows were not written", word);
   return ISM_OK;
 }
 

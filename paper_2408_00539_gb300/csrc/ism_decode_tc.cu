@@ -133,6 +133,7 @@ struct DecWalk {
 // the combine of the step before advanced them on other SMs and is complete, so
 // they are right in L2, whatever an SM's L1 holds.
 __device__ __forceinline__ int32_t cached(const DecodeArgs& a, int b) { return ld_gpu(a.cache_len + b); }
+__device__ __forceinline__ int32_t cached_len(const DecodeArgs& a, int b) { return bounded_len(cached(a, b), a.len_most); }
 
 // The boxes of 16 rows, [first, second), that hold the visible keys of the item's
 // tile j (kWin): those of the sinks, from the window's first key on, up to the last.
@@ -172,7 +173,7 @@ __device__ __forceinline__ DecWalk dec_walk(const DecodeArgs& a) {
     // a sequence a lane (every warp of every CTA reads the same few lines of L2:
     // with four a lane, in order, 40 ragged caches took 0.7 us a step more)
     const int b = base + lane;
-    const int n = b < a.batch ? dec_alloc_tiles(a, dec_tiles<kWin>(a, cached(a, b))) * row_heads : 0;
+    const int n = b < a.batch ? dec_alloc_tiles(a, dec_tiles<kWin>(a, cached_len(a, b))) * row_heads : 0;
     int incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -199,7 +200,7 @@ __device__ __forceinline__ DecWalk dec_walk(const DecodeArgs& a) {
     w.b = 0;
     w.end = w.t;
   }
-  w.len = cached(a, w.b) + 1;
+  w.len = cached_len(a, w.b) + 1;
   const int per_head = dec_alloc_tiles(a, dec_tiles<kWin>(a, w.len - 1));
   if (w.t >= sb + row_heads * per_head) w.end = w.t;
   w.g = w.t < w.end ? (w.t - sb) / per_head : 0;
@@ -220,7 +221,7 @@ __device__ __forceinline__ bool dec_next(const DecodeArgs& a, DecWalk& w, DecIte
     x.b = (int)(rest % a.batch);
     x.slot = (int)(rest / a.batch);
     x.k0 = x.slot * a.chunk;
-    if (x.b != w.b) w.len = cached(a, w.b = x.b) + 1;
+    if (x.b != w.b) w.len = cached_len(a, w.b = x.b) + 1;
     x.k1 = min(w.len, x.k0 + a.chunk);
     x.nsub = x.k1 > x.k0 ? (x.k1 - x.k0 + 127) / 128 : 0;
     x.nt = (x.nsub + kSub - 1) / kSub;
@@ -235,7 +236,7 @@ __device__ __forceinline__ bool dec_next(const DecodeArgs& a, DecWalk& w, DecIte
         if (++w.g == a.hkv / a.lanes) {
           w.g = 0;
           if (++w.b >= a.batch) return false;
-          w.len = cached(a, w.b) + 1;
+          w.len = cached_len(a, w.b) + 1;
         }
         continue;
       }

@@ -41,6 +41,7 @@ struct WinDecodeArgs {
   int64_t cap;
   const float *rope_cos, *rope_sin;
   int32_t* cache_len;
+  uint32_t* status;
   float scale;
   int32_t batch, hq, hkv, group;
   int32_t page_shift;  // log2 of the page size, or -1
@@ -139,7 +140,9 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 4 && G <= 4) || G <= 2
   auto row_of = [&](int key) -> int {  // (caches have below 2^31 rows)
     if (!a.pages.table) return (int)(b * a.cap) + key;
     const int page = a.page_shift >= 0 ? key >> a.page_shift : key / a.pages.page_size;
-    return a.pages.table[(int64_t)b * a.pages.max_pages + page] * a.pages.page_size + (key - page * a.pages.page_size);
+    // (an entry outside the pool: page_row)
+    const uint32_t entry = (uint32_t)a.pages.table[(int64_t)b * a.pages.max_pages + page];
+    return (int)min(entry, (uint32_t)a.pages.num_pages - 1u) * a.pages.page_size + (key - page * a.pages.page_size);
   };
   auto part_of = [&](const void* cache, int row) {
     return reinterpret_cast<const uint4*>(static_cast<const T*>(cache) + row * row_elems + g * D) + sub;
@@ -387,7 +390,9 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 4 && G <= 4) || G <= 2
   const int own_row = row_of(c);
   uint4* const k_row = const_cast<uint4*>(part_of(a.k_cache, own_row));
   uint4* const v_row = const_cast<uint4*>(part_of(a.v_cache, own_row));
-  for (int key = c + rank * (kThreads / LK) + threadIdx.x / LK; key < end; key += ranks * (kThreads / LK)) {
+  const bool held = !a.pages.table || page_held(a.pages, *page_entry(a.pages, b, c));
+  if (!held && threadIdx.x == 0) atomicOr(a.status, kStatusCache);
+  for (int key = c + rank * (kThreads / LK) + threadIdx.x / LK; held && key < end; key += ranks * (kThreads / LK)) {
     if (key == c) *k_row = k_own;
     v_row[(key - c) * (row_elems / N)] = key == c ? reinterpret_cast<const uint4*>(new_v)[sub] : make_uint4(0u, 0u, 0u, 0u);
   }
@@ -506,7 +511,7 @@ cudaError_t launch_decode_window(const DecodeArgs& d, const void* k_new, const v
   a.q = d.q; a.k_new = k_new; a.v_new = v_new;
   a.k_cache = const_cast<void*>(d.k_cache); a.v_cache = const_cast<void*>(d.v_cache);
   a.out = d.out; a.lse = d.lse; a.pages = d.pages; a.cap = d.cap;
-  a.rope_cos = rope_cos; a.rope_sin = rope_sin; a.cache_len = d.cache_len; a.scale = d.scale;
+  a.rope_cos = rope_cos; a.rope_sin = rope_sin; a.cache_len = d.cache_len; a.status = d.status; a.scale = d.scale;
   a.batch = d.batch; a.hq = d.hq; a.hkv = d.hkv; a.group = d.group; a.win = d.win;
   a.page_shift = -1;
   if (d.pages.table && (d.pages.page_size & (d.pages.page_size - 1)) == 0)

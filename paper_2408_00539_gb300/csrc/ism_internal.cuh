@@ -38,13 +38,19 @@ __device__ __forceinline__ int32_t ld_gpu(const int32_t* p) {
 // b start at b * cap (append kernels) or at Tile::k_base (attention kernels).
 struct KvPages {
   const int32_t* table;
-  int32_t page_size, max_pages;
+  int32_t page_size, max_pages, num_pages;
 };
 __device__ __forceinline__ const int32_t* page_entry(const KvPages& pg, int b, int64_t p) {
-  return pg.table + (int64_t)b * pg.max_pages + p / pg.page_size;
+  return pg.table + (int64_t)b * pg.max_pages + (uint32_t)p / (uint32_t)pg.page_size;  // (positions are below 2^31)
+}
+// The host checks the entries on its own copy of the table; one outside the pool
+// (-1 where no page is held) stands for the last page here, so that whatever the
+// device's table holds, reads stay in the pool.  Writes ask page_held first.
+__device__ __forceinline__ bool page_held(const KvPages& pg, int32_t entry) {
+  return (uint32_t)entry < (uint32_t)pg.num_pages;
 }
 __device__ __forceinline__ int64_t page_row(const KvPages& pg, int32_t entry, int64_t p) {
-  return (int64_t)entry * pg.page_size + p % pg.page_size;
+  return (int64_t)min((uint32_t)entry, (uint32_t)pg.num_pages - 1u) * pg.page_size + (uint32_t)p % (uint32_t)pg.page_size;
 }
 // (A plain load of the table: dependent kernels read it behind their wait.)
 __device__ __forceinline__ int64_t paged_row(const KvPages& pg, int b, int64_t p) {
@@ -129,7 +135,7 @@ struct Meta {
 };
 
 // Status word bits recorded by device code.
-enum : uint32_t { kStatusTimeout = 1u, kStatusSmemAlign = 2u };
+enum : uint32_t { kStatusTimeout = 1u, kStatusSmemAlign = 2u, kStatusCache = 4u };
 
 // ---------------------------------------------------------------- dependent launches
 // A kernel launched as a programmatic dependent overlaps its launch and set-up
@@ -209,10 +215,22 @@ struct AppendPlan {
   int32_t* pair_order;
   int32_t* counter;  // set to zero (the forward's work counter)
 };
-// cache_len: lengths before the append (read only; the attention kernels
-// advance them).  snap_out (nullable): receives a copy of them.
+// The lengths before an append, on the device.  The host checks its mirror of
+// them; `most` is the longest length that leaves room for the new rows (and, with
+// rotary tables, for their positions).  A length outside [0, most] counts as the
+// nearest one inside, so that no kernel leaves the caches, the page table or the
+// rotary tables whatever the device holds; nothing is written for its sequence, and
+// the status word says so.
+struct CacheLens {
+  const int32_t* len;
+  int32_t most;
+  uint32_t* status;
+};
+__device__ __forceinline__ int32_t bounded_len(int32_t len, int32_t most) { return min(max(len, 0), most); }
+// lens: read only here; the attention kernels advance them.  snap_out (nullable):
+// receives a copy of them, bounded.
 cudaError_t launch_cache_write(int dtype, int batch, int l_new, int hkv, int d, int64_t cap, const KvPages& pages,
-                               const int32_t* cache_len, const void* k_new, const void* v_new,
+                               const CacheLens& lens, const void* k_new, const void* v_new,
                                void* k_cache, void* v_cache, const AppendPlan& plan, cudaStream_t st,
                                int32_t* snap_out);
 // Cache write with the rotary encoding of the new queries and keys (bf16
@@ -220,7 +238,7 @@ cudaError_t launch_cache_write(int dtype, int batch, int l_new, int hkv, int d, 
 // cache, rotated queries into q_rot [batch * l_new, hq, d], all in the cache's
 // type: bf16, or e4m3 (dtype ISM_E4M3) after division by the descales.
 cudaError_t launch_rope_cache_write(int dtype, int batch, int l_new, int hq, int hkv, int d, int64_t cap,
-                                   const KvPages& pages, const int32_t* cache_len, const void* q_new,
+                                   const KvPages& pages, const CacheLens& lens, const void* q_new,
                                    const void* k_new, const void* v_new, const float* cos_t, const float* sin_t,
                                    float q_descale, float k_descale, float v_descale, void* q_rot, void* k_cache,
                                    void* v_cache, const AppendPlan& plan, cudaStream_t st, int32_t* snap_out);
@@ -291,7 +309,7 @@ struct AttnArgs {
   // Append-prefill: the cache lengths [adv_batch], advanced by adv_len by the
   // forward kernel (the kernels before it read them; it does not).
   int32_t* adv_cache_len;
-  int32_t adv_batch, adv_len;
+  int32_t adv_batch, adv_len, adv_most;  // adv_most: as CacheLens::most
   // Rotary encoding (tensor-core backward only): when rope_cos is set, the dQ
   // and dK epilogues store the gradients of the unrotated queries and keys,
   // applying the transposed rotation of the row's position in its sequence
@@ -350,7 +368,8 @@ __device__ __forceinline__ int32_t q_tile_at(const AttnArgs& a, int64_t pos) {
 // Called by every thread of every block of a forward kernel.
 __device__ __forceinline__ void advance_cache_len(const AttnArgs& a) {
   if (a.adv_cache_len && blockIdx.x == 0)
-    for (int b = threadIdx.x; b < a.adv_batch; b += blockDim.x) a.adv_cache_len[b] += a.adv_len;
+    for (int b = threadIdx.x; b < a.adv_batch; b += blockDim.x)
+      a.adv_cache_len[b] = bounded_len(a.adv_cache_len[b], a.adv_most) + a.adv_len;
 }
 cudaError_t launch_simt_fwd(const AttnArgs& a, cudaStream_t st);
 cudaError_t launch_simt_bwd(const AttnArgs& a, cudaStream_t st);
@@ -363,7 +382,7 @@ struct DecodeArgs {
   KvPages pages;         // table == nullptr: contiguous caches
   void* out;             // [B, Hq, D]
   float* lse;            // [Hq, B] or null
-  const int32_t* c_snap; // cache length before the append, per sequence
+  const int32_t* c_snap; // cache length before the append, per sequence (bounded)
   int32_t batch, hq, hkv, d, dtype;
   int32_t group;         // query heads per KV head (the kernels pad it to a power of two)
   float qk_descale, v_descale;  // e4m3: dequantisation of the scores and of the output
@@ -390,7 +409,8 @@ struct DecodeArgs {
   int32_t q_written;     // the queries come from the cache write (rotated)
   int32_t* start;
   uint32_t* status;      // device status word (bounded waits)
-  int32_t* cache_len;    // [B] equal to c_snap until the combine kernel advances it by one
+  int32_t* cache_len;    // [B] equal to c_snap (where inside its bounds) until the combine kernel advances it by one
+  int32_t len_most;      // as CacheLens::most
   Window win;            // window == 0: none; else the row holds the tiles that the new row visits (TileWalk)
 };
 // Keys one work item of the tensor-core decode covers at most (its scores of

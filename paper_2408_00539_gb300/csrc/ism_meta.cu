@@ -442,19 +442,33 @@ __device__ __forceinline__ int32_t chunk_kv_end(const AppendSegs& sg, int32_t j)
   return j + 1;
 }
 
+// Cached keys of sequence b (CacheLens).
+__device__ __forceinline__ int32_t cached_len(const CacheLens& lens, int b) { return bounded_len(lens.len[b], lens.most); }
+// The row that key p of sequence b is written to (contiguous caches: from b * cap,
+// else through the page table), -1 where the sequence has no room (`len`: its
+// length as the device has it) or the page is not in the pool.
+__device__ __forceinline__ int64_t write_row(const CacheLens& lens, const KvPages& pages, int64_t cap, int b, int32_t len,
+                                             int64_t p) {
+  if ((uint32_t)len > (uint32_t)lens.most) return -1;
+  if (!pages.table) return (int64_t)b * cap + p;
+  const int32_t entry = *page_entry(pages, b, p);
+  const int64_t row = page_row(pages, entry, p);
+  return page_held(pages, entry) ? row : -1;
+}
+
 // The append plan's share of one thread (grid-stride; see AppendPlan).
-__device__ __forceinline__ void append_plan_part(const AppendPlan& p, int batch, const int32_t* cache_len) {
+__device__ __forceinline__ void append_plan_part(const AppendPlan& p, int batch, const CacheLens& lens) {
   if (!p.qtiles) return;
   const AppendSegs& sg = p.segs;
   const int32_t Ln = sg.l_new;
   const int64_t t0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, stride = (int64_t)gridDim.x * blockDim.x;
   if (t0 == 0) *p.counter = 0;
   for (int64_t i = t0; i < (int64_t)batch * Ln; i += stride)
-    p.kv_end[i] = cache_len[i / Ln] + chunk_kv_end(sg, (int32_t)(i % Ln));
+    p.kv_end[i] = cached_len(lens, (int)(i / Ln)) + chunk_kv_end(sg, (int32_t)(i % Ln));
   const int nqt = (Ln + p.bm - 1) / p.bm, npt = (nqt + 1) / 2;
   for (int64_t g = t0; g < (int64_t)batch * nqt; g += stride) {
     const int b = (int)(g / nqt), t = (int)(g % nqt);
-    const int32_t c = cache_len[b], r0 = t * p.bm, rl = min(Ln, r0 + p.bm) - 1;
+    const int32_t c = cached_len(lens, b), r0 = t * p.bm, rl = min(Ln, r0 + p.bm) - 1;
     Tile w;
     w.q_base = b * Ln; w.k_base = (int32_t)(b * p.kbase_stride);
     w.q_len = Ln; w.k_len = c + Ln; w.tile = t;
@@ -468,7 +482,7 @@ __device__ __forceinline__ void append_plan_part(const AppendPlan& p, int batch,
   }
 }
 
-// K_new/V_new rows into the caches at [c_snap[b], c_snap[b] + l_new) (rows of
+// K_new/V_new rows into the caches at [c, c + l_new) of the c cached keys (rows of
 // sequence b from b * cap, or through the page table).
 // The attention kernels read keys in tiles of 128 from key 0, so the last
 // tile of a sequence runs past its last key.  Masked keys get P = 0, but the
@@ -480,17 +494,17 @@ __device__ __forceinline__ void append_plan_part(const AppendPlan& p, int batch,
 // not multiplied.
 // The cache write also lays out the chunk's plan (one launch less: 3.4 us of
 // the 60 us of a 40-token append over 3000 keys were a one-block plan kernel).
-// It reads the cache lengths themselves (c_snap = cache_len): they stay as
-// they are until the attention kernel after it advances them, and single-token
-// steps find a copy in snap_out.
-__device__ __forceinline__ void copy_snapshot(int batch, const int32_t* c_snap, int32_t* snap_out) {
+// It reads the cache lengths themselves: they stay as they are until the
+// attention kernel after it advances them, and single-token steps find a copy in
+// snap_out.
+__device__ __forceinline__ void copy_snapshot(int batch, const CacheLens& lens, int32_t* snap_out) {
   if (!snap_out) return;
   for (int64_t b = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; b < batch; b += (int64_t)gridDim.x * blockDim.x)
-    snap_out[b] = c_snap[b];
+    snap_out[b] = cached_len(lens, b);
 }
 
 __device__ __forceinline__ void zero_value_tail(int batch, int l_new, int vec_per_row, int64_t cap,
-                                                const KvPages& pages, const int32_t* c_snap,
+                                                const KvPages& pages, const CacheLens& lens,
                                                 uint4* v_cache) {
   const int64_t total = (int64_t)batch * 128 * vec_per_row;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total;
@@ -498,13 +512,14 @@ __device__ __forceinline__ void zero_value_tail(int batch, int l_new, int vec_pe
     const int64_t row = i / vec_per_row;
     const int col = (int)(i % vec_per_row);
     const int b = (int)(row / 128);
-    const int64_t end = (int64_t)c_snap[b] + l_new;
+    const int32_t len = lens.len[b];
+    const int64_t end = (int64_t)bounded_len(len, lens.most) + l_new;
     const int64_t p = end + row % 128;
     int64_t stop = (end + 127) / 128 * 128;
     if (!pages.table && stop > cap) stop = cap;
     if (p >= stop) continue;
-    const int64_t dst = (pages.table ? paged_row(pages, b, p) : (int64_t)b * cap + p) * vec_per_row + col;
-    v_cache[dst] = make_uint4(0u, 0u, 0u, 0u);
+    const int64_t dst = write_row(lens, pages, cap, b, len, p);
+    if (dst >= 0) v_cache[dst * vec_per_row + col] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
@@ -514,14 +529,16 @@ __device__ __forceinline__ void zero_value_tail(int batch, int l_new, int vec_pe
 // e4m3 8 x 16384 keys 50.7 -> 48 (with the decode reading the old keys while
 // the new row is written).  Inputs are not __restrict__: nothing may be loaded
 // before the wait.
-__global__ void cache_write_kernel(int batch, int l_new, int row_bytes, int64_t cap, KvPages pages,
-                                   const int32_t* c_snap, const uint4* k_new,
+// (Blocks to an SM: the registers of six; with five, which two registers more leave
+// room for, 40 paged caches took 1 us a step longer.)
+__global__ void __launch_bounds__(256, 6) cache_write_kernel(int batch, int l_new, int row_bytes, int64_t cap, KvPages pages,
+                                   const CacheLens lens, const uint4* k_new,
                                    const uint4* v_new, uint4* k_cache, uint4* v_cache,
                                    const __grid_constant__ AppendPlan plan, int32_t* snap_out) {
   pdl_wait();
-  append_plan_part(plan, batch, c_snap);
+  append_plan_part(plan, batch, lens);
   const int vec_per_row = row_bytes / 16;
-  copy_snapshot(batch, c_snap, snap_out);
+  copy_snapshot(batch, lens, snap_out);
   const int64_t total = (int64_t)batch * l_new * vec_per_row;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total;
        i += (int64_t)gridDim.x * blockDim.x) {
@@ -529,18 +546,24 @@ __global__ void cache_write_kernel(int batch, int l_new, int row_bytes, int64_t 
     int col = (int)(i % vec_per_row);
     int b = (int)(row / l_new);
     int j = (int)(row % l_new);
-    const int64_t p = (int64_t)c_snap[b] + j;
-    int64_t dst = (pages.table ? paged_row(pages, b, p) : (int64_t)b * cap + p) * vec_per_row + col;
-    k_cache[dst] = k_new[i];
-    v_cache[dst] = v_new[i];
+    const uint4 k = k_new[i], v = v_new[i];  // (on their way while the length and the page are)
+    const int32_t len = lens.len[b];
+    int64_t dst = write_row(lens, pages, cap, b, len, (int64_t)bounded_len(len, lens.most) + j);
+    if (dst < 0) {
+      atomicOr(lens.status, kStatusCache);
+      continue;
+    }
+    dst = dst * vec_per_row + col;
+    k_cache[dst] = k;
+    v_cache[dst] = v;
   }
-  zero_value_tail(batch, l_new, vec_per_row, cap, pages, c_snap, v_cache);
+  zero_value_tail(batch, l_new, vec_per_row, cap, pages, lens, v_cache);
 }
 
 // Rotary encoding fused with the cache write.  One thread takes eight
 // consecutive coordinates k0..k0+7 of the first half of one head row and
 // their partners k0+D/2.. (a query head, a key head, or a value head, which
-// is copied as is).  Position of new token j of sequence b: c_snap[b] + j.
+// is copied as is).  New token j of sequence b sits behind its cached keys and j more.
 // The rotation is in fp32; the results are rounded once to the cache's type:
 // bf16, or e4m3 after division by the tensor's dequantisation factor
 // (q_descale for the rotated queries, k_descale / v_descale for the cache).
@@ -578,16 +601,16 @@ __device__ __forceinline__ void store8(void* base, int64_t elem, const float (&x
 }
 
 template <bool kE4M3>
-__global__ void rope_cache_write_kernel(int batch, int l_new, int hq, int hkv, int d, int64_t cap, KvPages pages,
-                                        const int32_t* c_snap, const __nv_bfloat16* q_new,
+__global__ void __launch_bounds__(256, 5) rope_cache_write_kernel(int batch, int l_new, int hq, int hkv, int d, int64_t cap, KvPages pages,
+                                        const CacheLens lens, const __nv_bfloat16* q_new,
                                         const __nv_bfloat16* k_new,
                                         const __nv_bfloat16* v_new, const float* cos_t,
                                         const float* sin_t, float q_descale, float k_descale,
                                         float v_descale, void* q_rot, void* k_cache, void* v_cache,
                                         const __grid_constant__ AppendPlan plan, int32_t* snap_out) {
   pdl_wait();
-  append_plan_part(plan, batch, c_snap);
-  copy_snapshot(batch, c_snap, snap_out);
+  append_plan_part(plan, batch, lens);
+  copy_snapshot(batch, lens, snap_out);
   const int half = d / 2;
   const int units = half / 8;  // 8-coordinate units in one half of a head row
   const int per_row = (hq + 2 * hkv) * units;
@@ -599,8 +622,11 @@ __global__ void rope_cache_write_kernel(int batch, int l_new, int hq, int hkv, i
     const int head = r / units;
     const int k0 = (r % units) * 8;
     const int b = (int)(row / l_new);
-    const int64_t p = (int64_t)c_snap[b] + row % l_new;
-    const int64_t dst_row = pages.table ? paged_row(pages, b, p) : (int64_t)b * cap + p;
+    const int32_t len = lens.len[b];
+    const int64_t p = (int64_t)bounded_len(len, lens.most) + row % l_new;
+    const int64_t dst_row = head < hq ? 0 : write_row(lens, pages, cap, b, len, p);
+    const bool write = dst_row >= 0;
+    if (!write) atomicOr(lens.status, kStatusCache);
     const __nv_bfloat16* src;
     void* dst;
     int64_t off;  // element offset of the head row in dst
@@ -621,8 +647,10 @@ __global__ void rope_cache_write_kernel(int batch, int l_new, int hq, int hkv, i
       float lo[8], hi[8];
       load8(src + k0, lo);
       load8(src + half + k0, hi);
-      store8<kE4M3>(v_cache, off + k0, lo, v_descale);
-      store8<kE4M3>(v_cache, off + half + k0, hi, v_descale);
+      if (write) {
+        store8<kE4M3>(v_cache, off + k0, lo, v_descale);
+        store8<kE4M3>(v_cache, off + half + k0, hi, v_descale);
+      }
       continue;
     }
     float lo[8], hi[8], c[8], s[8];
@@ -639,10 +667,12 @@ __global__ void rope_cache_write_kernel(int batch, int l_new, int hq, int hkv, i
       ol[e] = lo[e] * c[e] - hi[e] * s[e];
       oh[e] = hi[e] * c[e] + lo[e] * s[e];
     }
-    store8<kE4M3>(dst, off + k0, ol, descale);
-    store8<kE4M3>(dst, off + half + k0, oh, descale);
+    if (write) {
+      store8<kE4M3>(dst, off + k0, ol, descale);
+      store8<kE4M3>(dst, off + half + k0, oh, descale);
+    }
   }
-  zero_value_tail(batch, l_new, hkv * d * (kE4M3 ? 1 : 2) / 16, cap, pages, c_snap, reinterpret_cast<uint4*>(v_cache));
+  zero_value_tail(batch, l_new, hkv * d * (kE4M3 ? 1 : 2) / 16, cap, pages, lens, reinterpret_cast<uint4*>(v_cache));
 }
 
 }  // namespace
@@ -705,7 +735,7 @@ cudaError_t launch_write(void (*kern)(Params...), int64_t total, cudaStream_t st
 }  // namespace
 
 cudaError_t launch_cache_write(int dtype, int batch, int l_new, int hkv, int d, int64_t cap, const KvPages& pages,
-                               const int32_t* c_snap, const void* k_new, const void* v_new,
+                               const CacheLens& lens, const void* k_new, const void* v_new,
                                void* k_cache, void* v_cache, const AppendPlan& plan, cudaStream_t st,
                                int32_t* snap_out) {
   int elem = dtype == ISM_BF16 ? 2 : dtype == ISM_E4M3 ? 1 : 4;
@@ -714,12 +744,12 @@ cudaError_t launch_cache_write(int dtype, int batch, int l_new, int hkv, int d, 
   if (total == 0) return cudaSuccess;
   const int64_t tail = (int64_t)batch * 128 * (row_bytes / 16);  // value rows zeroed past the new end
   if (tail > total) total = tail;
-  return launch_write(cache_write_kernel, total, st, batch, l_new, row_bytes, cap, pages, c_snap, (const uint4*)k_new,
+  return launch_write(cache_write_kernel, total, st, batch, l_new, row_bytes, cap, pages, lens, (const uint4*)k_new,
                       (const uint4*)v_new, (uint4*)k_cache, (uint4*)v_cache, plan, snap_out);
 }
 
 cudaError_t launch_rope_cache_write(int dtype, int batch, int l_new, int hq, int hkv, int d, int64_t cap,
-                                   const KvPages& pages, const int32_t* c_snap, const void* q_new,
+                                   const KvPages& pages, const CacheLens& lens, const void* q_new,
                                    const void* k_new, const void* v_new, const float* cos_t, const float* sin_t,
                                    float q_descale, float k_descale, float v_descale, void* q_rot, void* k_cache,
                                    void* v_cache, const AppendPlan& plan, cudaStream_t st, int32_t* snap_out) {
@@ -729,7 +759,7 @@ cudaError_t launch_rope_cache_write(int dtype, int batch, int l_new, int hq, int
   const int64_t tail = (int64_t)batch * 128 * (hkv * d * (e4m3 ? 1 : 2) / 16);  // value rows zeroed past the new end
   if (tail > total) total = tail;
   return launch_write(e4m3 ? rope_cache_write_kernel<true> : rope_cache_write_kernel<false>, total, st, batch, l_new, hq,
-                      hkv, d, cap, pages, c_snap, (const __nv_bfloat16*)q_new, (const __nv_bfloat16*)k_new,
+                      hkv, d, cap, pages, lens, (const __nv_bfloat16*)q_new, (const __nv_bfloat16*)k_new,
                       (const __nv_bfloat16*)v_new, cos_t, sin_t, q_descale, k_descale, v_descale, q_rot, k_cache,
                       v_cache, plan, snap_out);
 }

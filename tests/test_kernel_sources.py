@@ -96,3 +96,30 @@ def test_metadata_is_read_as_it_was_written():
     nothing of theirs counts as constant."""
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "ism_meta.cu")).read())
     assert "__restrict__" not in text and "__ldg" not in text
+
+
+def _source(name):
+    return re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+
+
+def test_lengths_and_pages_on_the_device_are_bounded():
+    """What an append reads on the device (cache lengths, page entries) is not what
+    the host has checked: every use of it goes through a bound, and rows that do
+    not fit are not written."""
+    meta, tc, common = _source("ism_meta.cu"), _source("ism_decode_tc.cu"), _source("ism_internal.cuh")
+    assert not re.search(r"c_snap\s*\[|cache_len\s*\[", meta)
+    assert sorted(re.findall(r"[^\n]*lens\.len\[[^\n]*", meta)) == [
+        "    const int32_t len = lens.len[b];"] * 3 + [
+        "__device__ __forceinline__ int32_t cached_len(const CacheLens& lens, int b) "
+        "{ return bounded_len(lens.len[b], lens.most); }"]
+    row = _body(meta, meta.index("write_row("))
+    assert "lens.most) return -1" in row and "page_held(pages, entry) ? row : -1" in row
+    for name in ("cache_write_kernel", "rope_cache_write_kernel"):
+        body = next(b for n, _, b in KERNELS if n == name)
+        assert "write_row(lens" in body and "bounded_len(len, lens.most)" in body and "paged_row(" not in body
+    assert "bounded_len(len, lens.most)" in _body(meta, meta.index("void zero_value_tail("))
+    assert "write_row(lens" in _body(meta, meta.index("void zero_value_tail("))
+    assert len(re.findall(r"\bcached\(", tc)) == 2 and "bounded_len(cached(a, b), a.len_most)" in tc
+    assert "bounded_len(" in _body(common, common.index("advance_cache_len("))
+    assert "num_pages" in _body(common, common.index("page_row("))
+    assert "num_pages" in _body(_source("ism_decode_win.cu"), _source("ism_decode_win.cu").index("auto row_of"))
