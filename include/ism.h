@@ -519,8 +519,12 @@ ism_status_t ism_attn_prefill_append_e4m3_rope(const ism_attn_shape_t* shape, in
  *   new chunk or a single token.  Of the cache only the 128-key tiles that hold
  *   a visible key are read: of a block table, the entries of pages that end at
  *   or before the first new row's window and start at or past the sinks may be
- *   anything (-1 where ism_pages_trim has freed them).  A single token may take
- *   the cache lengths from cache_len_host alone.  Workspaces:
+ *   anything (-1 where ism_pages_trim has freed them).  What a call reads and
+ *   writes follows from cache_len_host as much as from cache_len (a single token
+ *   of a few sequences goes by cache_len_host alone, and so does what a captured
+ *   one replays; other forms go by cache_len within what cache_len_host laid
+ *   out), so the two must hold the same lengths: where they do not, the results
+ *   are undefined and ism_check_status reports ISM_ERR_INVALID_ARG.  Workspaces:
  *   ism_attn_prefill_append_workspace_size / _rope_workspace_size.
  * Errors: as the calls they extend, plus ISM_ERR_INVALID_ARG for a NULL window,
  * window < 1 or sinks < 0, and ISM_ERR_UNSUPPORTED for e4m3 inputs.
@@ -623,7 +627,7 @@ ism_status_t ism_pages_compact(const ism_pages_t* pages, int32_t* pages_used, is
  * word.  Returns ISM_ERR_TIMEOUT if any kernel gave up a bounded wait since
  * the last check (the kernel exits early and its outputs are undefined),
  * ISM_ERR_INVALID_ARG if an append found cache lengths or pages on the device
- * that its host mirrors do not have and left rows out, ISM_ERR_CUDA on a CUDA
+ * that its host mirrors do not have (see the appends), ISM_ERR_CUDA on a CUDA
  * error, ISM_OK otherwise. */
 ism_status_t ism_check_status(ism_stream_t stream);
 

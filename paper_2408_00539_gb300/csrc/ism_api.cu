@@ -1197,7 +1197,9 @@ ism_status_t append_impl(const ism_attn_shape_t* shape, int32_t batch, const voi
   const bool paged = cg.pages.table != nullptr;
   int64_t keys_most = cg.max_keys < INT32_MAX ? cg.max_keys : INT32_MAX;
   if (rope && rope->rows < keys_most) keys_most = rope->rows;
-  const CacheLens lens{cache_len, (int32_t)(keys_most - l_new), status};
+  uint32_t sum = 0;
+  for (int b = 0; window && b < batch; ++b) sum += lens_sum(cache_len_host[b], b);
+  const CacheLens lens{cache_len, (int32_t)(keys_most - l_new), status, window != nullptr, sum};
 
   // decode kernels serve up to kMaxDecodeGroup query heads per KV head; larger
   // groups take the forward kernels (one query row per tile)
@@ -1672,7 +1674,7 @@ ism_status_t ism_check_status(ism_stream_t stream) {
     return fail(ISM_ERR_CUDA, "a kernel found its shared memory misaligned and skipped its work (0x%x)", word);
   if (word & kStatusCache)
     return fail(ISM_ERR_INVALID_ARG, "an append found a cache length or a page on the device that the host's mirrors do not "
-                "have (0x%x): its rows were not written", word);
+                "have (0x%x)", word);
   return ISM_OK;
 }
 

@@ -221,11 +221,19 @@ struct AppendPlan {
 // nearest one inside, so that no kernel leaves the caches, the page table or the
 // rotary tables whatever the device holds; nothing is written for its sequence, and
 // the status word says so.
+// mirrored: the call goes by both the host's lengths and the device's (windows), so
+// they have to be the same; `sum` is the host's lens_sum, and a device with another
+// one goes into the status word too.
 struct CacheLens {
   const int32_t* len;
   int32_t most;
   uint32_t* status;
+  bool mirrored;
+  uint32_t sum;
 };
+// A sequence's share of the sum of a batch's lengths (an odd factor each: no single
+// length changes unnoticed, nor all by as much).
+__host__ __device__ __forceinline__ uint32_t lens_sum(int32_t len, int32_t b) { return (uint32_t)len * (2u * b + 1u); }
 __device__ __forceinline__ int32_t bounded_len(int32_t len, int32_t most) { return min(max(len, 0), most); }
 // lens: read only here; the attention kernels advance them.  snap_out (nullable):
 // receives a copy of them, bounded.

@@ -444,6 +444,24 @@ __device__ __forceinline__ int32_t chunk_kv_end(const AppendSegs& sg, int32_t j)
 
 // Cached keys of sequence b (CacheLens).
 __device__ __forceinline__ int32_t cached_len(const CacheLens& lens, int b) { return bounded_len(lens.len[b], lens.most); }
+// A mirrored cache write has one block more, the first: it compares the device's
+// lengths with the host's (beside the writes of another block that took 0.3 us a
+// step).  The other blocks' threads are numbered from 0.
+__device__ __forceinline__ bool check_mirror(const CacheLens& lens, int batch) {
+  if (!lens.mirrored || blockIdx.x > 0) return false;
+  if (threadIdx.x < 32) {
+    uint32_t sum = 0;
+    for (int b = threadIdx.x; b < batch; b += 32) sum += lens_sum(cached_len(lens, b), b);
+    if (__reduce_add_sync(0xffffffffu, sum) != lens.sum && threadIdx.x == 0) atomicOr(lens.status, kStatusCache);
+  }
+  return true;
+}
+__device__ __forceinline__ int64_t write_thread(const CacheLens& lens) {
+  return (int64_t)(blockIdx.x - lens.mirrored) * blockDim.x + threadIdx.x;
+}
+__device__ __forceinline__ int64_t write_threads(const CacheLens& lens) {
+  return (int64_t)(gridDim.x - lens.mirrored) * blockDim.x;
+}
 // The row that key p of sequence b is written to (contiguous caches: from b * cap,
 // else through the page table), -1 where the sequence has no room (`len`: its
 // length as the device has it) or the page is not in the pool.
@@ -461,7 +479,7 @@ __device__ __forceinline__ void append_plan_part(const AppendPlan& p, int batch,
   if (!p.qtiles) return;
   const AppendSegs& sg = p.segs;
   const int32_t Ln = sg.l_new;
-  const int64_t t0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, stride = (int64_t)gridDim.x * blockDim.x;
+  const int64_t t0 = write_thread(lens), stride = write_threads(lens);
   if (t0 == 0) *p.counter = 0;
   for (int64_t i = t0; i < (int64_t)batch * Ln; i += stride)
     p.kv_end[i] = cached_len(lens, (int)(i / Ln)) + chunk_kv_end(sg, (int32_t)(i % Ln));
@@ -499,7 +517,7 @@ __device__ __forceinline__ void append_plan_part(const AppendPlan& p, int batch,
 // snap_out.
 __device__ __forceinline__ void copy_snapshot(int batch, const CacheLens& lens, int32_t* snap_out) {
   if (!snap_out) return;
-  for (int64_t b = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; b < batch; b += (int64_t)gridDim.x * blockDim.x)
+  for (int64_t b = write_thread(lens); b < batch; b += write_threads(lens))
     snap_out[b] = cached_len(lens, b);
 }
 
@@ -507,8 +525,7 @@ __device__ __forceinline__ void zero_value_tail(int batch, int l_new, int vec_pe
                                                 const KvPages& pages, const CacheLens& lens,
                                                 uint4* v_cache) {
   const int64_t total = (int64_t)batch * 128 * vec_per_row;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * blockDim.x) {
+  for (int64_t i = write_thread(lens); i < total; i += write_threads(lens)) {
     const int64_t row = i / vec_per_row;
     const int col = (int)(i % vec_per_row);
     const int b = (int)(row / 128);
@@ -536,12 +553,12 @@ __global__ void __launch_bounds__(256, 6) cache_write_kernel(int batch, int l_ne
                                    const uint4* v_new, uint4* k_cache, uint4* v_cache,
                                    const __grid_constant__ AppendPlan plan, int32_t* snap_out) {
   pdl_wait();
+  if (check_mirror(lens, batch)) return;
   append_plan_part(plan, batch, lens);
   const int vec_per_row = row_bytes / 16;
   copy_snapshot(batch, lens, snap_out);
   const int64_t total = (int64_t)batch * l_new * vec_per_row;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * blockDim.x) {
+  for (int64_t i = write_thread(lens); i < total; i += write_threads(lens)) {
     int64_t row = i / vec_per_row;
     int col = (int)(i % vec_per_row);
     int b = (int)(row / l_new);
@@ -609,14 +626,14 @@ __global__ void __launch_bounds__(256, 5) rope_cache_write_kernel(int batch, int
                                         float v_descale, void* q_rot, void* k_cache, void* v_cache,
                                         const __grid_constant__ AppendPlan plan, int32_t* snap_out) {
   pdl_wait();
+  if (check_mirror(lens, batch)) return;
   append_plan_part(plan, batch, lens);
   copy_snapshot(batch, lens, snap_out);
   const int half = d / 2;
   const int units = half / 8;  // 8-coordinate units in one half of a head row
   const int per_row = (hq + 2 * hkv) * units;
   const int64_t total = (int64_t)batch * l_new * per_row;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * blockDim.x) {
+  for (int64_t i = write_thread(lens); i < total; i += write_threads(lens)) {
     const int64_t row = i / per_row;  // b * l_new + j
     const int r = (int)(i % per_row);
     const int head = r / units;
@@ -724,13 +741,13 @@ cudaError_t launch_pass_meta(const SegsDev& s, int32_t* kv_end, int bm, int bn, 
 }
 
 namespace {
-// A cache-write kernel over `total` threads.
+// A cache-write kernel over `total` threads (and a block for check_mirror).
 template <class... Params, class... Args>
-cudaError_t launch_write(void (*kern)(Params...), int64_t total, cudaStream_t st, Args... args) {
+cudaError_t launch_write(void (*kern)(Params...), int64_t total, bool mirrored, cudaStream_t st, Args... args) {
   int64_t grid = (total + 255) / 256;
   const int64_t top = (int64_t)sm_count() * 16;
   if (grid > top) grid = top;
-  return launch(true, kern, grid, 256, 0, st, args...);
+  return launch(true, kern, grid + mirrored, 256, 0, st, args...);
 }
 }  // namespace
 
@@ -744,7 +761,7 @@ cudaError_t launch_cache_write(int dtype, int batch, int l_new, int hkv, int d, 
   if (total == 0) return cudaSuccess;
   const int64_t tail = (int64_t)batch * 128 * (row_bytes / 16);  // value rows zeroed past the new end
   if (tail > total) total = tail;
-  return launch_write(cache_write_kernel, total, st, batch, l_new, row_bytes, cap, pages, lens, (const uint4*)k_new,
+  return launch_write(cache_write_kernel, total, lens.mirrored, st, batch, l_new, row_bytes, cap, pages, lens, (const uint4*)k_new,
                       (const uint4*)v_new, (uint4*)k_cache, (uint4*)v_cache, plan, snap_out);
 }
 
@@ -758,8 +775,8 @@ cudaError_t launch_rope_cache_write(int dtype, int batch, int l_new, int hq, int
   const bool e4m3 = dtype == ISM_E4M3;
   const int64_t tail = (int64_t)batch * 128 * (hkv * d * (e4m3 ? 1 : 2) / 16);  // value rows zeroed past the new end
   if (tail > total) total = tail;
-  return launch_write(e4m3 ? rope_cache_write_kernel<true> : rope_cache_write_kernel<false>, total, st, batch, l_new, hq,
-                      hkv, d, cap, pages, lens, (const __nv_bfloat16*)q_new, (const __nv_bfloat16*)k_new,
+  return launch_write(e4m3 ? rope_cache_write_kernel<true> : rope_cache_write_kernel<false>, total, lens.mirrored, st, batch,
+                      l_new, hq, hkv, d, cap, pages, lens, (const __nv_bfloat16*)q_new, (const __nv_bfloat16*)k_new,
                       (const __nv_bfloat16*)v_new, cos_t, sin_t, q_descale, k_descale, v_descale, q_rot, k_cache,
                       v_cache, plan, snap_out);
 }

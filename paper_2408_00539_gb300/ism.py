@@ -624,7 +624,8 @@ def prefill_append_window(q_new, k_new, v_new, k_cache, v_cache, cache_len, cach
     """``prefill_append`` (with rope=(cos, sin) ``prefill_append_rope``) under a
     sliding window: new token j of sequence b sees, of the keys it sees there,
     those from position cache_len[b] + j - window + 1 on and the first `sinks`.
-    Only those are read.  Returns (o_new, lse [Hq,B,Ln])."""
+    Only those are read.  cache_len_host must hold the device's lengths
+    (``check_status`` reports where it does not).  Returns (o_new, lse [Hq,B,Ln])."""
     _contig(q_new, k_new, v_new, k_cache, v_cache, cache_len)
     return _append("ism_attn_prefill_append_window", 0 if rope is None else _FORM_ROPE, _dtype_code(q_new), q_new,
                    k_new, v_new, k_cache, v_cache, cache_len, cache_len_host, new_seg_end, new_seg_type, softmax_scale,

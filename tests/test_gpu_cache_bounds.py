@@ -125,3 +125,44 @@ def test_pages_outside_the_pool(knobs, D, dtype, hq, hkv, entry, rope, n, one_la
         assert torch.equal(c[kept], before[kept])
     assert torch.equal(pairs[1][1][2 * page + 12:2 * page + 12 + n], x[2][1])
     assert torch.isfinite(o[1].float()).all()
+
+
+@pytest.mark.parametrize("one_launch", [0, 1])
+@pytest.mark.parametrize("n", [1, 5])
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("page", [0, 128])
+@pytest.mark.parametrize("D,dtype,hq,hkv", FORMS)
+def test_a_mirror_that_is_not_the_devices_is_reported(knobs, D, dtype, hq, hkv, page, rope, n, one_launch):
+    """Under a window, whichever form runs: both lengths fit the caches, so nothing else would show it."""
+    if rope and dtype != torch.bfloat16:
+        pytest.skip("rotary appends take bf16")
+    knobs("ISM_DECODE_WINDOW", one_launch)
+    B, cap = 40, 256
+    caches = [torch.zeros((B * cap, hkv, D), dtype=dtype, device=DEV) for _ in range(2)]
+    x = [torch.ones((B, n, h, D), dtype=dtype, device=DEV) for h in (hq, hkv, hkv)]
+    tables = tuple(torch.from_numpy(t).to(DEV) for t in wl.rope_tables(cap, D)) if rope else None
+    table = np.arange(2 * B, dtype=np.int32).reshape(B, 2)
+
+    def step(device, host):
+        dev = torch.from_numpy(device.copy()).to(DEV)
+        args = (dev, host, [n], [1], D ** -0.5, 60, 3)
+        if page:
+            ism.prefill_append_paged_window(*x, *caches, page, torch.from_numpy(table).to(DEV), table, *args, rope=tables)
+        else:
+            ism.prefill_append_window(*x, *(c.view(B, cap, hkv, D) for c in caches), *args, rope=tables)
+
+    lens = np.random.default_rng(n).integers(0, cap - n, B).astype(np.int32)
+    lens[:3] = 0, 100, cap - n - 1
+    ism.check_status(DEV)
+    step(lens, lens)
+    ism.check_status(DEV)
+    one, swapped = lens.copy(), lens.copy()
+    one[1] -= 1
+    swapped[1:3] = lens[2], lens[1]
+    for other in (one, np.maximum(lens - 1, 0), swapped):
+        step(lens, other)
+        with pytest.raises(ism.IsmError, match="the host's mirrors do not have") as info:
+            ism.check_status(DEV)
+        assert info.value.code == 1
+    step(lens, lens)
+    ism.check_status(DEV)
