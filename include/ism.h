@@ -586,6 +586,9 @@ ism_status_t ism_attn_prefill_append_paged_window(const ism_attn_shape_t* shape,
  *   of sequence src[i] (keys NULL: of all).  Full pages are shared, entries that
  *   were trimmed stay -1, and the rows of a last, partly filled page are copied
  *   into a free page, so that appends to either sequence write pages of its own.
+ *   At fewer keys than a trimmed source holds, the window that ends there may
+ *   reach pages that ism_pages_trim gave up: the fork is refused where the page of
+ *   its last key is one of them, and appends to dst are where they need another.
  *   A source may be listed several times, a destination once, and no sequence
  *   is both.
  * ism_pages_free: the listed sequences give up their pages and become empty; a
@@ -598,8 +601,8 @@ ism_status_t ism_attn_prefill_append_paged_window(const ism_attn_shape_t* shape,
  *   among the first n, in ascending order.  Rows that hold keys are copied; the
  *   entries of every sequence follow.  *pages_used (nullable) = n.
  * Errors: ISM_ERR_INVALID_ARG for malformed pools, lists, tables or counts, too
- * few free pages, a fork from a trimmed page or into a sequence that is not
- * empty.
+ * few free pages, a fork at fewer keys than the source holds whose last key's
+ * page was trimmed, or into a sequence that is not empty.
  * ------------------------------------------------------------------------- */
 typedef struct {
   void *k_pool, *v_pool;

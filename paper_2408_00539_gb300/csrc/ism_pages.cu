@@ -273,10 +273,11 @@ ism_status_t ism_pages_fork(const ism_pages_t* pages, const int32_t* src_host, c
         if (b.row(d)[k] >= 0) return bad("destination %lld is not empty", d);
       const int32_t keys = keys_host ? keys_host[i] : b.len(s);
       if (keys < 0 || keys > b.len(s)) return bad("sequence %lld: a fork at %lld of %lld keys", s, keys, b.len(s));
-      if (keys % p.page_size) {
-        if (b.row(s)[keys / p.page_size] < 0) return bad("sequence %lld: the page of key %lld has been freed", s, keys - 1);
-        ++need;
-      }
+      // (of all keys the last page may be gone: a window of one key does not see it)
+      const bool behind = keys > 0 && (keys < b.len(s) || keys % p.page_size);
+      if (behind && b.row(s)[(keys - 1) / p.page_size] < 0)
+        return bad("sequence %lld: the page of key %lld has been freed", s, keys - 1);
+      need += keys % p.page_size != 0;
       entries += keys / p.page_size + 2;
     }
     if ((r = b.check_free(need)) != ISM_OK) return r;

@@ -800,7 +800,9 @@ class PagedCache:
 
     def fork(self, src, dst, keys=None):
         """Empty slot dst[i] becomes a copy of slot src[i] (of its first keys[i]
-        keys): full pages are shared, a partly filled last page is copied."""
+        keys): full pages are shared, a partly filled last page is copied.  At
+        fewer keys than a trimmed slot holds, the window there may need pages that
+        are gone: refused where the last key's page is, else by the appends."""
         s, n, _kept_s = _host_array(src, np.int32, "i")
         d, nd, _kept_d = _host_array(dst, np.int32, "i")
         k, nk, _kept_k = (None, n, None) if keys is None else _host_array(keys, np.int32, "i")

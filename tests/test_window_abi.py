@@ -141,3 +141,35 @@ def test_python_arguments():
         make(n=lens.long())
     with pytest.raises(ValueError, match="32-bit"):
         ism._window(2 ** 31, 0)
+
+
+@host_only
+def test_forks_from_pages_given_up_are_refused(lib):
+    """At fewer keys than the source holds, also where they end with a page: what the
+    window ending there needs has been given up.  At all of its keys a fork is as
+    good as the source."""
+    def fork(length, table, keys, page=128):
+        held = sorted(p for p in table if p >= 0)
+        table = np.array([table, [-1] * len(table)], np.int32)
+        lens, refs = np.array([length, 0], np.int32), np.zeros(8, np.int32)
+        refs[held] = 1
+        s = ism._PAGES.pack(FAKE, FAKE, 64, 8, page, 2, table.shape[1], FAKE, ism._addr(table), FAKE, ism._addr(lens),
+                            ism._addr(refs))
+        src, dst, n = np.array([0], np.int32), np.array([1], np.int32), np.array([keys], np.int32)
+        before = table.copy(), lens.copy(), refs.copy()
+        code = lib.ism_pages_fork(s, ism._addr(src), ism._addr(dst), ism._addr(n), 1, None)
+        if code == 1:
+            assert all((a == b).all() for a, b in zip(before, (table, lens, refs)))
+        return code, lib.ism_last_error().decode()
+
+    passed = 3  # past the checks, at the launch: there is no device
+    for keys in (1, 127, 128, 129, 255, 256):
+        assert fork(500, [-1, -1, 4, 5], keys) == (1, f"sequence 0: the page of key {keys - 1} has been freed")
+    for keys in (257, 384, 385, 500):
+        assert fork(500, [-1, -1, 4, 5], keys)[0] == passed
+    for keys in (128, 100, 385, 512):  # with a page of sinks
+        assert fork(512, [0, -1, -1, 5], keys)[0] == passed
+    for keys in (129, 256, 384):
+        assert fork(512, [0, -1, -1, 5], keys)[0] == 1
+    assert fork(512, [-1, -1, -1, -1], 512)[0] == passed  # (a window of one key)
+    assert fork(512, [-1, -1, -1, -1], 511)[0] == fork(512, [-1, -1, -1, -1], 384)[0] == 1
