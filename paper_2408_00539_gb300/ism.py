@@ -832,7 +832,13 @@ class PagedCache:
         """``prefill_append_paged`` (or its windowed or rotary form) of one chunk to
         each of the slots [first, first + batch); takes the pages that the new
         rows need and advances the mirrors."""
+        if not q_new.dtype == k_new.dtype == v_new.dtype == self.k_pool.dtype:
+            raise TypeError("the new rows must be of the pools' type")
         B, Ln = q_new.shape[:2]
+        heads = self.k_pool.shape[1:]
+        if q_new.dim() != 4 or not (B, Ln, *heads) == tuple(k_new.shape) == tuple(v_new.shape) or \
+                q_new.shape[3] != heads[-1]:
+            raise ValueError("q_new must be [B, Ln, Hq, D] and k_new, v_new [B, Ln, Hkv, D] of the pools' heads")
         rows = slice(first, first + B)
         self.reserve(range(first, first + B), Ln)
         args = (q_new, k_new, v_new, self.k_pool, self.v_pool, self.page_size, self.block_table[rows],

@@ -173,3 +173,27 @@ def test_forks_from_pages_given_up_are_refused(lib):
         assert fork(512, [0, -1, -1, 5], keys)[0] == 1
     assert fork(512, [-1, -1, -1, -1], 512)[0] == passed  # (a window of one key)
     assert fork(512, [-1, -1, -1, -1], 511)[0] == fork(512, [-1, -1, -1, -1], 384)[0] == 1
+
+
+@host_only
+def test_appends_that_do_not_fit_the_pools_are_refused():
+    """Types and heads of the new rows against the pools', before a page is taken."""
+    pool = torch.zeros((256, 2, 64), dtype=torch.bfloat16)
+    refs = np.zeros(2, np.int32)
+    cache = ism.PagedCache(pool, pool.clone(), 128, torch.full((2, 3), -1, dtype=torch.int32),
+                           np.full((2, 3), -1, np.int32), torch.zeros(2, dtype=torch.int32), np.zeros(2, np.int32), refs)
+
+    def rows(hq=4, hk=2, hv=2, d=64, n=1, nk=None, b=1, dtype=torch.bfloat16, kd=None, vd=None):
+        return (torch.zeros((b, n, hq, d), dtype=dtype), torch.zeros((b, nk or n, hk, d), dtype=kd or dtype),
+                torch.zeros((b, nk or n, hv, d), dtype=vd or dtype))
+
+    f32, f8 = torch.float32, torch.float8_e4m3fn
+    for bad in (rows(dtype=f32), rows(dtype=f8), rows(kd=f32), rows(vd=f32)):
+        with pytest.raises(TypeError, match="pools"):
+            cache.append(*bad, [1], [1], 0.1)
+    for bad in (rows(hk=4, hv=4), rows(hk=1, hv=1), rows(hv=4), rows(d=128), rows(nk=2)):
+        with pytest.raises(ValueError, match="pools"):
+            cache.append(*bad, [1], [1], 0.1, window=20)
+    with pytest.raises(ValueError):
+        cache.append(*(x[0] for x in rows()), [1], [1], 0.1)
+    assert not refs.any() and (cache.block_table_host == -1).all() and not cache.cache_len_host.any()
