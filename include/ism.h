@@ -503,8 +503,11 @@ ism_status_t ism_attn_prefill_append_e4m3_rope(const ism_attn_shape_t* shape, in
  * A query token thus sees the window of keys up to itself, the rest of its own
  * query segment, and the sinks; every row sees itself.  No counterpart in the
  * paper; with window + sinks of at least the longest sequence (of an append:
- * cached and new keys) it is the plain operation, by the same kernels except in
- * the bf16 backward at head_dim 128, whose windowed kernels round once less.
+ * cached and new keys) it is the plain operation, by the same kernels and with
+ * their results bit for bit, except in two forms: the bf16 backward at head_dim
+ * 128, whose windowed kernels round once less, and single tokens that run in one
+ * launch (up to 8 query heads a KV head: bf16 of few sequences, fp32 of up to 768),
+ * where P stays in fp32 and sums are in another order.
  *   window >= 1, sinks >= 0; ISM_BF16 or ISM_FP32, head_dim 64 or 128.
  *   rope: NULL, or the rotary tables of the calls' rotary forms.
  *

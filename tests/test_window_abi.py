@@ -197,3 +197,11 @@ def test_appends_that_do_not_fit_the_pools_are_refused():
     with pytest.raises(ValueError):
         cache.append(*(x[0] for x in rows()), [1], [1], 0.1)
     assert not refs.any() and (cache.block_table_host == -1).all() and not cache.cache_len_host.any()
+
+
+def test_the_header_names_what_differs_from_the_plain_calls():
+    """A window that hides nothing runs the plain calls' kernels but in two forms; both stand there."""
+    text = open(os.path.join(ROOT, "include", "ism.h")).read()
+    said = re.search(r"it is the plain operation(.*?)\n \*   window >= 1", text, re.S).group(1)
+    said = re.sub(r"\s*\n \*\s*", " ", said)
+    assert "bf16 backward at head_dim 128" in said and "single tokens" in said
