@@ -440,11 +440,15 @@ cudaError_t launch_t(const WinDecodeArgs& a, int ranks, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, decode_window_kernel<T, D, G>, a);
 }
 
-// Clusters of `ranks` blocks that run at a time (asked once a kernel and size; 0: unknown).
+// Clusters of `ranks` blocks that run at a time on the current device (asked once a
+// device, kernel and size, on devices past kMaxDevices each time; 0: unknown).
+constexpr int kMaxDevices = 64;
 template <typename T, int D, int G>
 int active_clusters(int ranks) {
-  static std::atomic<int> known[kMaxRanks + 1];
-  int n = known[ranks].load(std::memory_order_relaxed);
+  static std::atomic<int> known[kMaxDevices][kMaxRanks + 1];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
+  int n = dev < kMaxDevices ? known[dev][ranks].load(std::memory_order_relaxed) : 0;
   if (n > 0) return n;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(ranks * sm_count()));
@@ -459,7 +463,7 @@ int active_clusters(int ranks) {
     cudaGetLastError();
     return 0;
   }
-  known[ranks].store(n, std::memory_order_relaxed);
+  if (dev < kMaxDevices) known[dev][ranks].store(n, std::memory_order_relaxed);
   return n;
 }
 

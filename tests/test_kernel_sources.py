@@ -123,3 +123,11 @@ def test_lengths_and_pages_on_the_device_are_bounded():
     assert "bounded_len(" in _body(common, common.index("advance_cache_len("))
     assert "num_pages" in _body(common, common.index("page_row("))
     assert "num_pages" in _body(_source("ism_decode_win.cu"), _source("ism_decode_win.cu").index("auto row_of"))
+
+
+def test_what_is_asked_of_a_device_is_kept_a_device():
+    """The number of resident clusters sets the one-launch step's shape; it is the current device's."""
+    text = _source("ism_decode_win.cu")
+    body = _body(text, text.index("int active_clusters("))
+    assert "cudaGetDevice(&dev)" in body and re.findall(r"\bknown\[[^;]*\]\.(?:load|store)", body)
+    assert all(x.startswith("dev") for x in re.findall(r"\bknown\[(\w+)", body[body.index("cudaGetDevice"):]))
