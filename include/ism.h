@@ -652,7 +652,7 @@ ism_status_t ism_debug_timeout_probe(uint32_t spin_limit, ism_stream_t stream);
  * process so far (all threads). */
 enum {
   ISM_KERNEL_FWD = 1,        /* one-pass forward (and append-prefill over a chunk) */
-  ISM_KERNEL_BWD_DKDV = 2,   /* backward dK/dV */
+  ISM_KERNEL_BWD_DKDV = 2,   /* backward dK/dV (windows: with the sums of the sinks' parts) */
   ISM_KERNEL_BWD_DQ = 3,     /* backward dQ */
   ISM_KERNEL_BWD_PRE = 4,    /* backward preprocessing (Delta; bf16: the CUDA-core dQ kernel computes its own) */
   ISM_KERNEL_DECODE = 5,     /* single-token append (split-KV + merge) */

@@ -1268,7 +1268,6 @@ cudaError_t launch_bwd_t(const AttnArgs& a, int64_t k_rows, cudaStream_t st) {
     timer_begin(ISM_KERNEL_BWD_DKDV, st);
     e = launch(a.dependent, dkdv_kernel<kHD, kWin>, grid, kWin ? dkv::kThreadsWin : dkv::kThreads, dkv::Layout<kHD>::kSmemBytes, st, tq, tdo,
                          tk, tv, a);
-    timer_end(ISM_KERNEL_BWD_DKDV, st);
     count_launch();
     if (e != cudaSuccess) return e;
     if (kWin && a.parts.n > 0) {
@@ -1277,6 +1276,7 @@ cudaError_t launch_bwd_t(const AttnArgs& a, int64_t k_rows, cudaStream_t st) {
         return e;
       count_launch();
     }
+    timer_end(ISM_KERNEL_BWD_DKDV, st);
   }
   if (a.nq && a.ds) {
     timer_begin(ISM_KERNEL_BWD_DQ, st);

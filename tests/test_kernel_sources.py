@@ -131,3 +131,18 @@ def test_what_is_asked_of_a_device_is_kept_a_device():
     body = _body(text, text.index("int active_clusters("))
     assert "cudaGetDevice(&dev)" in body and re.findall(r"\bknown\[[^;]*\]\.(?:load|store)", body)
     assert all(x.startswith("dev") for x in re.findall(r"\bknown\[(\w+)", body[body.index("cudaGetDevice"):]))
+
+
+def test_timers_cover_every_launch_of_their_kind():
+    """The sums of the sinks' parts are part of dK/dV: no launch of the backward lies outside a timer."""
+    text = _source("ism_bwd_tc.cu")
+    body = _body(text, text.index("cudaError_t launch_bwd_t("))
+    within, launches = 0, 0
+    for m in re.finditer(r"timer_(begin|end)\(|\b(?:launch|launch_dkdv_pair|launch_dq_gemm)\(", body):
+        if m.group(1):
+            within += 1 if m.group(1) == "begin" else -1
+            assert within in (0, 1)
+        else:
+            launches += 1
+            assert within == 1, body[m.start():m.start() + 80]
+    assert launches == 6 and within == 0
