@@ -233,8 +233,8 @@ int64_t count_pairs(const ism_segments_t* s, const Window& win) {
 // exceeds 8.  A part is as long as the key tiles that hold no sink (those of the
 // window) and no shorter than a quarter of the share.  2 x 8192 tokens of 32 / 8
 // heads, window 1024 (sink tiles of 57 and 72 query tiles, a share 66): dK/dV 613 us
-// whole, 514 and 6 for the sums in parts (with the 57 whole a layer takes 30 us
-// more).  Three dialogues of 6001 tokens, 16 heads of 64, window 500 (up to 22, a
+// whole and 514 in parts when they were built (492 by now), the sums 6 (with the 57
+// whole a layer took 30 us more).  Three dialogues of 6001 tokens, 16 heads of 64, window 500 (up to 22, a
 // share 27): a layer 211 us whole, 226 in parts.
 SinkParts sink_parts(const ism_segments_t* s, const ism_attn_shape_t* sh, const Window& win) {
   SinkParts p{};

@@ -166,12 +166,15 @@ __device__ __forceinline__ int64_t unit_of(int64_t k, int64_t n_units) {
 // static walk.  Under a window, whose units are short, the producer publishes
 // them decoded and brings the rows' bounds close to the softmax warps: multi-head
 // 4 x 4096, window 2047, 380 -> 351 us; grouped-query 2 x 8192, window 1024, 242
-// -> 239; 24 dialogues, window 256, 130 -> 128.
+// -> 239; 24 dialogues, window 256, 130 -> 128 (calls in a row, metadata pass included).
 // kWin: a sliding window with sinks.  A unit visits the key tiles of the sinks in
 // front of its first row's window and then that window's (TileWalk); a row may
 // see nothing of a tile, so its maximum starts finite, as in a part of a split.
-// 2 x 8192 tokens of 32 / 8 heads, window 1024: 232 us (1160 TFLOP/s over the visible
-// pairs); one dialogue of 16384, 8 / 2 heads, window 4096: 164 us (1520).  Bound by the
+// 2 x 8192 tokens of 32 / 8 heads, window 1024: 232 us for the kernel alone, from cold
+// caches (1160 TFLOP/s over the visible pairs); one dialogue of 16384, 8 / 2 heads,
+// window 4096: 164 us (1520).  P enters P V as it does without a window, in bf16 at
+// head_dim 128 (relative error 0.0023, of which the output's rounding is 0.0017; 16
+// bits would double the steps of P V).  Bound by the
 // chain of a block, two of which are in flight: 1.40 us for a block of two heads that
 // every row sees in full, 1.82 with a mask, 2.5 a unit (fitted over windows of 1 to
 // 4000).  So neither leaving out the exponentials of 32 keys that no row of a warp

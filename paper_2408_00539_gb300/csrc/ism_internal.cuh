@@ -59,8 +59,9 @@ __device__ __forceinline__ int64_t paged_row(const KvPages& pg, int b, int64_t p
 
 // Sliding window and sinks: the row at position p of its sequence (cached keys
 // counted) sees, of the keys below its bound, those at p - window + 1 and later
-// and the first `sinks`.  window == 0: every key below the bound.  The host cuts
-// both to the longest sequence, so that sums of positions stay in 32 bits.
+// and the first `sinks`.  window == 0: every key below the bound.  The host drops a
+// window that hides nothing from its longest sequence, so window + sinks is less than
+// that one's length here and sums with positions stay in 32 bits.
 struct Window {
   int32_t window, sinks;
 };
