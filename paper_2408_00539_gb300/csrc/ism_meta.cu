@@ -101,9 +101,11 @@ __global__ void kv_end_kernel(SegsDev s, int32_t* kv_end) {
 // non-empty tiles; k-tile c is first reached by the q-tile holding the first
 // row whose kv_end exceeds c*bn.
 // `dyn` holds the per-sequence offsets ((num_seqs + 1) * 16 bytes).
+template <bool kWin>
 __device__ void tiles_body(const SegsDev& s, int bm, int bn, const int32_t* kv_end, int64_t nq,
                            int64_t nk, Tile* qtiles, Tile* ktiles, uint8_t* tile_class, int32_t* kt_full_end,
-                           int32_t* kt_end, int32_t* qt_begin, unsigned char* dyn, const Window& win) {
+                           int32_t* kt_end, int32_t* qt_begin, unsigned char* dyn, const Window& window) {
+  const Window win = kWin ? window : Window{0, 0};
   int64_t* toff = reinterpret_cast<int64_t*>(dyn);
   int32_t* qoff = reinterpret_cast<int32_t*>(toff + s.num_seqs + 1);
   int32_t* koff = qoff + s.num_seqs + 1;
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(256) tiles_kernel(SegsDev s, int bm, int bn, c
                              int64_t nq, int64_t nk, Tile* qtiles, Tile* ktiles, uint8_t* tile_class,
                              int32_t* kt_full_end, int32_t* kt_end, int32_t* qt_begin) {
   extern __shared__ __align__(16) unsigned char dyn[];
-  tiles_body(s, bm, bn, kv_end, nq, nk, qtiles, ktiles, tile_class, kt_full_end, kt_end, qt_begin, dyn, Window{0, 0});
+  tiles_body<false>(s, bm, bn, kv_end, nq, nk, qtiles, ktiles, tile_class, kt_full_end, kt_end, qt_begin, dyn, Window{0, 0});
 }
 
 // Work lists ordered by decreasing cost (counting sort, one block).  Cost of
@@ -193,9 +195,11 @@ __device__ __forceinline__ bool pair_head(const Tile* qtiles, int64_t nq, int64_
 // pairs_first: q_order lists the pair heads of the third list first (in its
 // order), then the odd-indexed q-tiles; the forward of an odd group at
 // head_dim 64 reads its pairs from there.
+template <bool kWin>
 __device__ void order_body(const Tile* qtiles, int64_t nq, const Tile* ktiles, int64_t nk,
                            int max_cost, int32_t* q_order, int32_t* k_order, int32_t* pair_order, int32_t* hist,
-                           int32_t* kp_order, bool pairs_first, int bm, const Window& win) {
+                           int32_t* kp_order, bool pairs_first, int bm, const Window& window) {
+  const Window win = kWin ? window : Window{0, 0};
   int32_t heads = 0;  // pair heads listed at the front of q_order (pairs_first)
   for (int pass = 0; pass < 5; ++pass) {
     const bool keys = pass == 1 || pass == 3;
@@ -288,11 +292,13 @@ __device__ void sink_parts_body(const Tile* ktiles, int64_t nk, int bm, const Wi
 // (Eq. fj, a warp per segment), the q-/k-tile descriptors, the cost-ordered work lists and, for
 // the stored-dS backward, the pair offsets.  Global writes of one phase are
 // visible to the block's threads after __syncthreads.
+template <bool kWin>
 __global__ void __launch_bounds__(1024)
     pass_meta_kernel(SegsDev s, int32_t* kv_end, int bm, int bn, int64_t nq, int64_t nk, Tile* qtiles,
                      Tile* ktiles, int max_cost, int32_t* q_order, int32_t* k_order, int32_t* pair_order,
                      int32_t* kpair_off, int32_t* counters, int n_counters, int32_t* kp_order, bool pairs_first,
-                     Window win, SinkParts parts) {
+                     Window window, SinkParts parts) {
+  const Window win = kWin ? window : Window{0, 0};
   extern __shared__ __align__(16) unsigned char dyn[];
   pdl_wait();
   if ((int)threadIdx.x < n_counters) counters[threadIdx.x] = 0;  // work counters of the kernels that follow
@@ -307,12 +313,12 @@ __global__ void __launch_bounds__(1024)
     for (int32_t j = start + lane; j < end; j += 32) kv_end[base + j] = query ? end : j + 1;
   }
   __syncthreads();
-  tiles_body(s, bm, bn, kv_end, nq, nk, qtiles, ktiles, nullptr, nullptr, nullptr, nullptr, dyn, win);
+  tiles_body<kWin>(s, bm, bn, kv_end, nq, nk, qtiles, ktiles, nullptr, nullptr, nullptr, nullptr, dyn, win);
   __syncthreads();
-  order_body(qtiles, nq, ktiles, nk, max_cost, q_order, k_order, pair_order, reinterpret_cast<int32_t*>(dyn),
+  order_body<kWin>(qtiles, nq, ktiles, nk, max_cost, q_order, k_order, pair_order, reinterpret_cast<int32_t*>(dyn),
              kp_order, pairs_first, bm, win);
   if (kpair_off) pair_offsets_body(ktiles, nk, kpair_off);
-  if (parts.n > 0) sink_parts_body(ktiles, nk, bm, win, parts);
+  if (kWin && parts.n > 0) sink_parts_body(ktiles, nk, bm, win, parts);
 }
 
 // The same for a small batch (at most kSmallTiles tiles and sequences and
@@ -322,6 +328,8 @@ __global__ void __launch_bounds__(1024)
 // ranks are counted by comparing every pair of tiles.  The general pass goes
 // through global memory and some twenty block barriers of 1024 threads: one
 // dialogue of 256 tokens 8.0 us, this one 5.0; 2 x 8192 tokens 11.5 and 10.
+// kWin, in both: the windows' passes.  Plain ones with a window of 0 in the same code
+// took 0.7 us longer (8.5, three dialogues of 6001 tokens).
 constexpr int kSmallTiles = 256, kSmallSegs = 1024, kSmallThreads = 512;
 
 // How many of the n costs come before cost c of item i in the list (higher
@@ -336,10 +344,12 @@ __device__ __forceinline__ int rank_of(const int32_t* costs, int n, int32_t c, i
   return r;
 }
 
+template <bool kWin>
 __global__ void __launch_bounds__(kSmallThreads)
     pass_meta_small_kernel(SegsDev s, int32_t* kv_end, int bm, int nq, Tile* qtiles, Tile* ktiles, int32_t* q_order,
                            int32_t* k_order, int32_t* pair_order, int32_t* kpair_off, int32_t* counters,
-                           int n_counters, bool pairs_first, Window win, SinkParts parts) {
+                           int n_counters, bool pairs_first, Window window, SinkParts parts) {
+  const Window win = kWin ? window : Window{0, 0};
   __shared__ int32_t cu[kSmallTiles + 1], cseg[kSmallTiles + 1], off[kSmallTiles + 1], ends[kSmallSegs];
   __shared__ uint8_t types[kSmallSegs];
   // per list: q-tiles, k-tiles, pair heads, odd q-tiles; -1 where not listed
@@ -385,7 +395,7 @@ __global__ void __launch_bounds__(kSmallThreads)
     k.a1 = win_last_qtile(win, t, bm, L);
     cost[0][tid] = q_cost(q, q.a1, bm, win);
     cost[1][tid] = max(k.a1 - k.a0, 0);
-    end1[tid] = q.a1;
+    if (kWin) end1[tid] = q.a1;
   }
   __syncthreads();
   const bool odd = q.tile & 1;
@@ -393,9 +403,9 @@ __global__ void __launch_bounds__(kSmallThreads)
     // a pair costs what its second tile does (the first, when it has none)
     const bool second = tid + 1 < nq && !odd && (q.tile + 1) * bm < q.q_len;
     // (under a window the second one's key tiles start where the first one's do: its window no earlier)
-    cost[odd ? 3 : 2][tid] = odd      ? cost[0][tid]
-                             : second ? max(cost[0][tid], win.window ? q_cost(q, end1[tid + 1], bm, win) : end1[tid + 1])
-                                      : cost[0][tid];
+    const int own = q_cost(q, q.a1, bm, win);
+    cost[odd ? 3 : 2][tid] =
+        odd || !second ? own : max(own, kWin ? q_cost(q, end1[tid + 1], bm, win) : cost[0][tid + 1]);
   }
   __syncthreads();
   int32_t pairs;
@@ -426,7 +436,7 @@ __global__ void __launch_bounds__(kSmallThreads)
     const bool query = types[seg] == ISM_SEG_QUERY;
     for (int j = start + lane; j < end; j += 32) kv_end[cu[b] + j] = query ? end : j + 1;
   }
-  if (parts.n > 0) {
+  if (kWin && parts.n > 0) {
     __syncthreads();  // the tiles above
     sink_parts_body(ktiles, nq, bm, win, parts);
   }
@@ -724,19 +734,21 @@ cudaError_t launch_pass_meta(const SegsDev& s, int32_t* kv_end, int bm, int bn, 
                              cudaStream_t st, int32_t* kp_order, bool pairs_first, bool dependent, Window win,
                              SinkParts parts) {
   if (bm == bn && nq <= kSmallTiles && s.num_seqs <= kSmallTiles && s.num_segs <= kSmallSegs && !kp_order)
-    return launch(dependent, pass_meta_small_kernel, 1, kSmallThreads, 0, st, s, kv_end, bm, (int)nq, qtiles,
-                            ktiles, q_order, k_order, pair_order, kpair_off, counters, n_counters, pairs_first, win, parts);
+    return launch(dependent, win.window ? pass_meta_small_kernel<true> : pass_meta_small_kernel<false>, 1, kSmallThreads, 0,
+                  st, s, kv_end, bm, (int)nq, qtiles, ktiles, q_order, k_order, pair_order, kpair_off, counters, n_counters,
+                  pairs_first, win, parts);
   size_t a = (size_t)(s.num_seqs + 1) * (sizeof(int64_t) + 2 * sizeof(int32_t));
   size_t b = sizeof(int32_t) * (size_t)(max_cost + 1);
   size_t smem = a > b ? a : b;
+  auto kern = win.window ? pass_meta_kernel<true> : pass_meta_kernel<false>;
   // opted in well below 48 KB: the kernel's static shared memory (the block
   // scans' warp totals) and the dynamic part together must fit what a launch
   // gets without opting in
   if (smem > 16 * 1024) {
-    cudaError_t e = cudaFuncSetAttribute(pass_meta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
   }
-  return launch(dependent, pass_meta_kernel, 1, 1024, smem, st, s, kv_end, bm, bn, nq, nk, qtiles, ktiles, max_cost,
+  return launch(dependent, kern, 1, 1024, smem, st, s, kv_end, bm, bn, nq, nk, qtiles, ktiles, max_cost,
                           q_order, k_order, pair_order, kpair_off, counters, n_counters, kp_order, pairs_first, win, parts);
 }
 

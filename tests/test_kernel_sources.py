@@ -146,3 +146,14 @@ def test_timers_cover_every_launch_of_their_kind():
             launches += 1
             assert within == 1, body[m.start():m.start() + 80]
     assert launches == 6 and within == 0
+
+
+def test_plain_metadata_knows_no_window():
+    """The metadata kernels of plain calls are instantiations without the window's arithmetic (0.7 us a pass)."""
+    text = _source("ism_meta.cu")
+    for name in ("pass_meta_kernel", "pass_meta_small_kernel"):
+        at = text.index(name + "(")
+        assert re.search(r"template <bool kWin>\s+__global__[^;{]*$", text[:at]), name
+        body = next(b for n, _, b in KERNELS if n == name)
+        assert "kWin ? window : Window{0, 0}" in body and "if (kWin && parts.n > 0)" in body
+        assert re.search(name + r"<true>\s*:\s*" + name + "<false>", text)
