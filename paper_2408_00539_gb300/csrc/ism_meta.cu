@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(kSmallThreads)
     // a pair costs what its second tile does (the first, when it has none)
     const bool second = tid + 1 < nq && !odd && (q.tile + 1) * bm < q.q_len;
     // (under a window the second one's key tiles start where the first one's do: its window no earlier)
-    const int own = q_cost(q, q.a1, bm, win);
+    const int own = kWin ? cost[0][tid] : q.a1;
     cost[odd ? 3 : 2][tid] =
         odd || !second ? own : max(own, kWin ? q_cost(q, end1[tid + 1], bm, win) : cost[0][tid + 1]);
   }
